@@ -16,7 +16,7 @@
 // the row ends inside the CTA, otherwise by the CTA that comes last (or by decode_join.cu), in the order of the pieces in any case.
 //
 // Measured, device times of calls that take turns on three inputs: 128K tokens of 8 KV heads in bf16 86.0 us (6.2 TB/s, 96 % of the copy rate; reading
-// alone the memory gives up to 7.7 TB/s between the first tiles, 4 us, and the last), 48 requests of 500 to 32K tokens in e4m3 120.7 us (6.2 TB/s), one
+// alone the memory gives up to 7.7 TB/s between the first tiles, 4 us, and the last), 48 requests of 500 to 32K tokens in e4m3 122.2 us (6.2 TB/s), one
 // request of one token 5.4 us.
 #include <algorithm>
 
@@ -85,7 +85,6 @@ __global__ void __launch_bounds__(kThreads, 1) decode_attention_kernel(DecodePar
   using H = Half16<F16>;
   using HP = Half16<F16 || E4M3>;            // 8-bit caches are multiplied as f16, which holds their numbers exactly
   constexpr int kHeads = NT * 8, kSteps = D / 16;
-  constexpr bool kTwoTerms = !E4M3 || F16;   // of a weight (see there)
   // where a channel of a piece lies in shared memory: heads that are written together (two apart) in banks of their own
   auto piece_at = [](int head, int ch) { return head * D + (E4M3 ? ch ^ ((head & 2) << 3) ^ ((head & 4) >> 2) : ch ^ ((head & 6) << 2)); };
   extern __shared__ __align__(1024) char smem[];
@@ -481,9 +480,9 @@ __global__ void __launch_bounds__(kThreads, 1) decode_attention_kernel(DecodePar
       }
 #pragma unroll
       for (int u16 = 0; u16 < T::kSubs; ++u16) {
-        // Weights as two 16-bit terms, the second what rounding to the first leaves: one term alone would add 2^-9 (bf16) to the output's own rounding, and
-        // the second product costs nothing where memory is the bound.  Over an 8-bit cache it does cost something (48 ragged requests in a loop of seconds,
-        // 133 us), and for bf16 outputs one f16 term is enough: its 2^-11 disappear beside their 2^-8
+        // Weights as two 16-bit terms, the second what rounding to the first leaves: one term alone would add 2^-9 (bf16) or 2^-12 (f16) to the output's own
+        // rounding.  The second product costs nothing over a 16-bit cache, where memory is the bound, and little over an 8-bit one (one term and two, bf16 outputs: 48
+        // ragged requests 120.7 and 122.2 us, in a loop of seconds under the power cap 127.3 and 132.0; 128K tokens 49.7 and 53.5, with 16 heads a KV head 64 and 75)
         uint32_t big[NT][2], rest[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -494,11 +493,9 @@ __global__ void __launch_bounds__(kThreads, 1) decode_attention_kernel(DecodePar
             l[n][1] += w1;
             const typename HP::T2 hi = HP::narrow(w0, w1);
             big[n][i] = ptx::transpose_8x8(*reinterpret_cast<const uint32_t*>(&hi));
-            if constexpr (kTwoTerms) {
-              const float2 back = HP::widen(hi);
-              const typename HP::T2 lo = HP::narrow(w0 - back.x, w1 - back.y);
-              rest[n][i] = ptx::transpose_8x8(*reinterpret_cast<const uint32_t*>(&lo));
-            }
+            const float2 back = HP::widen(hi);
+            const typename HP::T2 lo = HP::narrow(w0 - back.x, w1 - back.y);
+            rest[n][i] = ptx::transpose_8x8(*reinterpret_cast<const uint32_t*>(&lo));
           }
         if constexpr (E4M3) {
           const int key = u16 * 16 + (lane & 15);
@@ -514,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_attention_kernel(DecodePar
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
                 ptx::mma_16x8x16<true>(o[n][j + i], a, big[n][0], big[n][1]);
-                if constexpr (kTwoTerms) ptx::mma_16x8x16<true>(o[n][j + i], a, rest[n][0], rest[n][1]);
+                ptx::mma_16x8x16<true>(o[n][j + i], a, rest[n][0], rest[n][1]);
               }
             }
           }

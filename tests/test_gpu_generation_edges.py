@@ -1,0 +1,67 @@
+"""Generation from a paged cache where it is easily wrong: sizes at a limit of the launch, numbers that are not finite, weights far below a row's largest."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import generation_oracle as O
+from tests.test_gpu_generation import BF16, E4M3, F16, ROUND, cosa, gpu, pools, tables, wide  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- attention
+def contents(lens, hq, hkv, d, page, dtype, cache, seed):
+    """q, pools, scales and table of a call with ordinary numbers, and the place of a token in the pools."""
+    rng, gen = np.random.default_rng(seed), torch.Generator(device="cuda").manual_seed(seed)
+    table, pages, _ = tables(lens, page, rng, spare=1)
+    k, v = ((torch.randn(pages, hkv, page, d, generator=gen, device="cuda") * (25.0 if cache is E4M3 else 1.0)).to(cache) for _ in range(2))
+    ks, vs = (torch.rand(hkv, generator=gen, device="cuda") * 0.05 + 0.01 for _ in range(2)) if cache is E4M3 else (None, None)
+    q = torch.randn(len(lens), hq, d, generator=gen, device="cuda").to(dtype)
+    return q, k, v, ks, vs, table
+
+
+def put(pool, table, page, b, h, tokens, channel, x):
+    """Writes x into one channel of some tokens."""
+    flat = pool.view(torch.uint8) if pool.dtype is E4M3 else pool
+    x = torch.tensor(x, device="cuda").to(pool.dtype)
+    x = x.view(torch.uint8) if pool.dtype is E4M3 else x
+    t = torch.as_tensor(list(tokens), device="cuda")
+    flat[gpu(table[b], torch.int64)[t // page], h, t % page, channel] = x
+
+
+def attend(cosa, q, k, v, ks, vs, table, lens, route):
+    handle = cosa.make_cache(k, v, gpu(table), k_scale=ks, v_scale=vs)
+    out, lse = torch.full_like(q, 9.0), torch.full(q.shape[:2], 9.0, device="cuda")
+    opt = cosa.decode_options(impl=int(route == "check"), ctas=1 if route == "one CTA" else 0)
+    if route == "workspace":      # the pieces are joined by a kernel of its own
+        space = torch.empty(cosa.cosa_decode_workspace_bytes(1, handle, q.shape[0], q.shape[1]), dtype=torch.uint8, device="cuda")
+        opt.workspace, opt.workspace_bytes = space.data_ptr(), space.numel()
+    cosa.cosa_decode_attention(handle, q, gpu(lens), out, lse, opt=opt)
+    assert cosa.cosa_device_status() == 0
+    return out, lse
+
+
+ROUTES = ["as usual", "one CTA", "workspace", "check"]
+
+
+@pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (F16, F16), (BF16, E4M3), (F16, E4M3)])
+@pytest.mark.parametrize("route", ROUTES)
+def test_weights_are_not_rounded(cosa, dtype, cache, route):
+    """Two tokens of opposite values, whose logits differ by little: the output is a small difference of the two weights, in which an error of
+    either stands out."""
+    hq, d, page = 64, 128, 8
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.zeros(1, hq, d, device="cuda")
+    q[0, :, 0] = torch.rand(hq, generator=gen, device="cuda") * 0.004 + 1e-4
+    q[0, :, 1] = 1.0
+    k, v = (torch.zeros(1, 1, page, d, device="cuda") for _ in range(2))
+    k[0, 0, 0, 0] = 1.0
+    v[0, 0, 0], v[0, 0, 1] = 1.0, -1.0
+    q, k, v = q.to(dtype), k.to(cache), v.to(cache)
+    ones = torch.ones(1, device="cuda") if cache is E4M3 else None
+    out, lse = attend(cosa, q, k, v, ones, ones, np.zeros((1, 1), np.int64), [2], route)
+    want, _, size = O.attention(wide(q[0]), wide(k)[0, 0, :2], wide(v)[0, 0, :2], d ** -0.5)
+    # (the bound for two 16-bit terms, with values of 1)
+    bad = np.abs(wide(out[0]) - want) - (ROUND[dtype] * np.abs(want) + 4 * 128 * 2.0 ** -24 * size + 2.0 ** -16 + 2.0 ** -25)
+    assert bad.max() <= 0, float(bad.max())
