@@ -171,7 +171,8 @@ SmemLimit g_limit;
 
 cudaError_t launch_page_plan(const PlanParams& p, cudaStream_t st) {
   const size_t smem = (size_t)p.batch * 16;
-  cudaError_t e = smem > 48 * 1024 ? raise_smem_limit((const void*)page_plan_kernel, &g_limit, smem) : cudaSuccess;
+  // (48 KB without asking are for this and the kernel's fixed half KB together)
+  cudaError_t e = smem > 40 * 1024 ? raise_smem_limit((const void*)page_plan_kernel, &g_limit, kMaxPlanRequests * 16) : cudaSuccess;
   if (e != cudaSuccess) return e;
   const int grid = std::max(1, std::min(device_sm_count(), (p.max_tokens + kTokensPerCta - 1) / kTokensPerCta));
   const auto at16 = [](const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; };

@@ -1,4 +1,7 @@
 """Generation from a paged cache where it is easily wrong: sizes at a limit of the launch, numbers that are not finite, weights far below a row's largest."""
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -8,6 +11,28 @@ from oracle import generation_oracle as O
 from tests.test_gpu_generation import BF16, E4M3, F16, ROUND, cosa, gpu, pools, tables, wide  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+# ---------------------------------------------------------------- page plan
+PLANS = """
+import numpy as np, paper_2607_25291_b200 as cosa
+from oracle import generation_oracle as O
+from tests.test_gpu_generation import check_plan
+for batch in (3041, 3042, 3043, 3044, 3060, 3071, 3072, 3073, 4000):
+    rng = np.random.default_rng(batch)
+    lens, grow = rng.integers(0, 20, batch), rng.choice([-1, 0, 1, 9], batch)
+    need = sum(O.pages_of(n + g, 8) - O.pages_of(n, 8) for n, g in zip(lens, grow) if g > 0)
+    check_plan(cosa, lens, grow, 8, 5, need // 2, int(grow.clip(0).sum()) + 1, 7, rng)
+    print("planned", batch)
+"""
+
+
+def test_page_plan_sizes_around_the_shared_memory_limit():
+    """In a process of its own, smaller batches first: a larger one would have raised the kernel's limit for all."""
+    run = subprocess.run([sys.executable, "-c", PLANS], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0, run.stdout[-500:] + run.stderr[-1500:]
+    assert "planned 4000" in run.stdout
 
 
 # ---------------------------------------------------------------- attention
