@@ -164,6 +164,11 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
+def _is_expanded(shape, strides) -> bool:
+    """Some dimension repeats the same elements.  The C calls take strides of zero for the dense layout, so that they would read past such a tensor."""
+    return any(n > 1 and s == 0 for n, s in zip(shape, strides))
+
+
 def make_shape(q: torch.Tensor, k: torch.Tensor, causal: bool = True, block: int = 128) -> CosaShape:
     """q [B,Hq,N,d], k [B,Hkv,N,d] (3-d tensors are taken as B = 1)."""
     b, hq, n, d = q.shape if q.dim() == 4 else (1, *q.shape)
@@ -392,6 +397,8 @@ def make_cache(k, v, page_table, bounds=None, k_scale=None, v_scale=None, page_s
             raise ValueError("page_size differs from the pools'")
         c.k, c.v = k.data_ptr(), v.data_ptr()
         if not k.is_contiguous():
+            if _is_expanded(k.shape, k.stride()):
+                raise ValueError("k, v: expanded tensors are no pools")
             c.strides = (ctypes.c_int64 * 3)(*k.stride()[:3])
         dtypes = [k.dtype] if k.dtype is not torch.float8_e4m3fn else [_BF16, torch.float16]
         c.cache_dtype = -1 if k.dtype is not torch.float8_e4m3fn else COSA_E4M3
@@ -449,7 +456,7 @@ def cosa_page_plan(page_table, page_size: int, lens, grow, free_ring, ring_state
 # (these calls are made once a layer and token, and a short one's kernels last no longer than its enqueue: what is asked of a tensor is
 # asked once, and options are built once for a set of values.  Python's share of a call 3.4 to 5.7 us -> 2.6 to 4.3)
 def _bad_rows(name, heads, d):
-    return ValueError(f"{name}: expected a [n,{heads or 'heads'},{d}] CUDA tensor with contiguous rows")
+    return ValueError(f"{name}: expected a [n,{heads or 'heads'},{d}] CUDA tensor with contiguous rows (not an expanded one)")
 
 
 def _rows(t: torch.Tensor, shape, name: str):
@@ -459,7 +466,7 @@ def _rows(t: torch.Tensor, shape, name: str):
     if t.is_contiguous():
         return t.data_ptr(), None
     s = t.stride()
-    if s[2] != 1:
+    if s[2] != 1 or _is_expanded(shape, s):
         raise _bad_rows(name, shape[1], shape[2])
     return t.data_ptr(), s[:2]
 

@@ -127,3 +127,50 @@ def test_binding_refusals(B):
         B.make_cache(t, t, torch.zeros(1, 2, dtype=torch.int32))      # not on the GPU
     with pytest.raises(ValueError):
         B.make_cache(None, None, torch.zeros(1, 2, dtype=torch.int32))      # neither pools nor bounds
+
+
+class OnGpu:
+    """A CPU tensor that says it is on the GPU, for checks that come before any use of its memory."""
+
+    is_cuda = True
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+class NoCalls:
+    """Stands for the library where nothing may reach it."""
+
+    def __getattr__(self, name):
+        def called(*args):
+            raise AssertionError(f"{name} was called")
+        return called
+
+
+def test_expanded_tensors_are_refused(B, monkeypatch):
+    """A tensor that repeats its elements (a stride of zero) is not handed on: the C calls would take it for a dense one and read, or write, past its end."""
+    import torch
+    monkeypatch.setattr(B, "_lib", NoCalls())
+    monkeypatch.setattr(B, "_stream_ptr", lambda stream: 0)
+    bf16, i32, d = torch.bfloat16, torch.int32, 128
+    new = lambda *shape, dtype=bf16: OnGpu(torch.zeros(*shape, dtype=dtype))      # noqa: E731
+    row, heads, tokens = (OnGpu(torch.zeros(*shape, dtype=bf16).expand(3, 4, d)) for shape in ((1, 1, d), (1, 4, d), (3, 1, d)))
+    table, lens, slots = new(3, 10, dtype=i32), new(3, dtype=i32), new(3, dtype=i32)
+    pool = new(5, 4, 16, d)
+    cache = B.make_cache(pool, pool, table, bounds=new(5, 4, 2, d))
+    pages, count = new(3, 4, 10, dtype=i32), new(3, 4, dtype=i32)
+    for bad in (row, heads, tokens):
+        for call in (lambda: B.cosa_decode_attention(cache, bad, lens, new(3, 4, d)), lambda: B.cosa_decode_attention(cache, new(3, 4, d), lens, bad),
+                     lambda: B.cosa_cache_append(cache, bad, bad, slots), lambda: B.cosa_decode_select(cache, bad, lens, 0.5, pages, count)):
+            with pytest.raises(ValueError):
+                call()
+    for shape in ((1, 1, 1, d), (5, 1, 1, d), (1, 4, 16, d), (5, 4, 1, d)):
+        bad = OnGpu(torch.zeros(*shape, dtype=bf16).expand(5, 4, 16, d))
+        with pytest.raises(ValueError):
+            B.make_cache(bad, bad, table)
+    # a dimension of one element may have any stride
+    one = torch.zeros(3, 8, d, dtype=bf16)[:, ::8].as_strided((3, 1, d), (8 * d, 0, 1))
+    assert B._rows(OnGpu(one), one.shape, "q")[1] == (8 * d, 0)
