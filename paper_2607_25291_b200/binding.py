@@ -164,11 +164,6 @@ def _stream_ptr(stream) -> int:
     return int(stream.cuda_stream)
 
 
-def _is_expanded(shape, strides) -> bool:
-    """Some dimension repeats the same elements.  The C calls take strides of zero for the dense layout, so that they would read past such a tensor."""
-    return any(n > 1 and s == 0 for n, s in zip(shape, strides))
-
-
 def make_shape(q: torch.Tensor, k: torch.Tensor, causal: bool = True, block: int = 128) -> CosaShape:
     """q [B,Hq,N,d], k [B,Hkv,N,d] (3-d tensors are taken as B = 1)."""
     b, hq, n, d = q.shape if q.dim() == 4 else (1, *q.shape)
@@ -202,6 +197,11 @@ _BF16, _I32, _F32 = torch.bfloat16, torch.int32, torch.float32
 _DENSE = (ctypes.c_int64 * 3)(0, 0, 0)
 
 
+def _is_expanded(shape, strides) -> bool:
+    """Some dimension repeats the same elements.  The C calls take strides of zero for the dense layout, so that they would read past such a tensor."""
+    return any(n > 1 and s == 0 for n, s in zip(shape, strides))
+
+
 def _strided_ptr(t: torch.Tensor, name: str):
     """Pointer and (batch, head, token) element strides of a [B,H,N,d] bf16 CUDA tensor or view whose rows are contiguous;
     _DENSE stands for the dense layout."""
@@ -210,8 +210,8 @@ def _strided_ptr(t: torch.Tensor, name: str):
         return t.data_ptr(), _DENSE
     if t.dim() == 3:
         t = t[None]                                         # [H,N,d]: one batch item
-    if not t.is_cuda or t.dtype != _BF16 or t.dim() != 4 or t.stride(3) != 1:
-        raise ValueError(f"{name}: expected a [B,H,N,d] CUDA bfloat16 tensor with contiguous rows")
+    if not t.is_cuda or t.dtype != _BF16 or t.dim() != 4 or t.stride(3) != 1 or _is_expanded(t.shape, t.stride()):
+        raise ValueError(f"{name}: expected a [B,H,N,d] CUDA bfloat16 tensor with contiguous rows (not an expanded one)")
     return t.data_ptr(), (_DENSE if t.is_contiguous() else (ctypes.c_int64 * 3)(*t.stride()[:3]))
 
 

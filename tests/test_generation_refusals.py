@@ -174,3 +174,25 @@ def test_expanded_tensors_are_refused(B, monkeypatch):
     # a dimension of one element may have any stride
     one = torch.zeros(3, 8, d, dtype=bf16)[:, ::8].as_strided((3, 1, d), (8 * d, 0, 1))
     assert B._rows(OnGpu(one), one.shape, "q")[1] == (8 * d, 0)
+
+
+def test_expanded_tensors_of_a_prompt_are_refused(B, monkeypatch):
+    """The same for the calls on a prompt, whose strides of zero stand for the dense layout too."""
+    import torch
+    monkeypatch.setattr(B, "_lib", NoCalls())
+    monkeypatch.setattr(B, "_set_strides", lambda opt, **kw: None)
+    monkeypatch.setattr(B, "_stream_ptr", lambda stream: 0)
+    new = lambda *shape, dtype=torch.bfloat16: OnGpu(torch.zeros(*shape, dtype=dtype))      # noqa: E731
+    lists = new(1, 4, 2, 2, dtype=torch.int32), new(1, 4, 2, dtype=torch.int32)
+    q, k, out = new(1, 4, 256, 128), new(1, 2, 256, 128), new(1, 4, 256, 128)
+    for heads, slot in ((4, 0), (2, 1), (4, 3)):
+        bad = OnGpu(torch.zeros(1, 1, 1, 128, dtype=torch.bfloat16).expand(1, heads, 256, 128).as_strided((1, heads, 256, 128), (0, 0, 0, 1)))
+        args = [q, k, k, out]
+        args[slot] = bad
+        if slot == 1:
+            args[2] = bad
+        with pytest.raises(ValueError):
+            B.cosa_osk_attention(args[0], args[1], args[2], *lists, 1.0, args[3])
+        if slot < 2:
+            with pytest.raises(ValueError):
+                B.cosa_kap_select(args[0], args[1], 0.5, *lists)
