@@ -457,8 +457,9 @@ int cosa_decode_select_ex(const cosa_cache* cache, const void* q, int32_t batch,
  *   count      in   [batch, hkv] entries of each list
  *   out        out  [batch, hq, d] of cache->dtype
  *   out_lse    out  [batch, hq] float32, may be NULL
- * Logits, maxima, sums and outputs are held in float32; the weights go into the second product as two 16-bit terms, as good as unrounded.  The result
- * does not depend on what else runs: partial results are joined in a fixed order.
+ * Logits, maxima, sums and outputs are held in float32; the weights go into the second product as two 16-bit terms, as good as unrounded (bf16: to
+ * 2^-17 of each; f16, which an 8-bit cache takes as well: to 2^-22, or 2^-40 of the row's largest).  The result does not depend on what else runs: partial
+ * results are joined in a fixed order.
  */
 int cosa_decode_attention(const cosa_cache* cache, const void* q, int32_t batch, int32_t hq, const int32_t* lens, const int32_t* pages,
                           const int32_t* count, int32_t list_stride, void* out, float* out_lse, void* stream);

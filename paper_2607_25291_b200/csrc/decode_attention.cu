@@ -85,6 +85,10 @@ __global__ void __launch_bounds__(kThreads, 1) decode_attention_kernel(DecodePar
   using H = Half16<F16>;
   using HP = Half16<F16 || E4M3>;            // 8-bit caches are multiplied as f16, which holds their numbers exactly
   constexpr int kHeads = NT * 8, kSteps = D / 16;
+  // Weights that are multiplied as f16 are taken against the maximum less 15, so that they reach up to 2^15: f16 ends at 2^16 and has no exponents below 2^-24, where
+  // weights of at most 1 would be lost behind a token 17 above them (2^-25 of the largest each, 0.4 % of a row of 128K tokens).  So they are not before 2^-40 of it.  `top`
+  // is the lowered maximum everywhere: outputs and sums of a row's pieces grow alike.  Logits beyond 2^22, which differ by halves, are left as they are
+  constexpr float kLift = F16 || E4M3 ? 15.f : 0.f;
   // where a channel of a piece lies in shared memory: heads that are written together (two apart) in banks of their own
   auto piece_at = [](int head, int ch) { return head * D + (E4M3 ? ch ^ ((head & 2) << 3) ^ ((head & 4) >> 2) : ch ^ ((head & 6) << 2)); };
   extern __shared__ __align__(1024) char smem[];
@@ -457,11 +461,12 @@ __global__ void __launch_bounds__(kThreads, 1) decode_attention_kernel(DecodePar
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float now = top[n][i];
+          float now = -INFINITY;
 #pragma unroll
           for (int u16 = 0; u16 < T::kSubs; ++u16) now = fmaxf(now, fmaxf(x[u16][n][i], x[u16][n][i + 2]));
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, off));
+          now = fmaxf(top[n][i], kLift && fabsf(now) < 0x1p22f ? now - kLift : now);
           ref[n][i] = now == -INFINITY ? 0.f : now;
           keep[n][i] = ptx::ex2_approx(top[n][i] - ref[n][i]);
           moved |= now != top[n][i];

@@ -71,6 +71,30 @@ ROUTES = ["as usual", "one CTA", "workspace", "check"]
 
 
 @pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (F16, F16), (BF16, E4M3), (F16, E4M3)])
+@pytest.mark.parametrize("n,d", [(40000, 64), (9001, 128)])
+@pytest.mark.parametrize("gap", [10.0, 16.0, 18.0, 26.0])
+@pytest.mark.parametrize("route", ["as usual", "one CTA", "check"])
+def test_many_small_weights_behind_a_large_one(cosa, dtype, cache, n, d, gap, route):
+    """One token's logit lies `gap` above all others, and its value is zero: the output is what the others' weights, e^-gap each, add up to."""
+    q, k, v = torch.zeros(1, 2, d, device="cuda"), torch.zeros(1, 1, n, d, device="cuda"), torch.rand(1, 1, n, d, device="cuda") + 0.5
+    q[0, :, 0] = 1.0
+    k[0, 0, 7, 0], v[0, 0, 7] = gap, 0.0
+    # (a multiple of 8 tokens a page, all in one order)
+    page, count = 8, -(-n // 8)
+    k, v = (torch.nn.functional.pad(x, (0, 0, 0, count * page - n)).view(count, page, 1, d).transpose(1, 2).to(cache).contiguous() for x in (k, v))
+    q, ones = q.to(dtype), torch.ones(1, device="cuda") if cache is E4M3 else None
+    handle = cosa.make_cache(k, v, gpu([range(count)]), k_scale=ones, v_scale=ones)
+    out, lse = torch.empty_like(q), torch.empty(1, 2, device="cuda")
+    cosa.cosa_decode_attention(handle, q, gpu([n]), out, lse, softmax_scale=1.0, opt=cosa.decode_options(impl=int(route == "check"), ctas=int(route == "one CTA")))
+    want, want_lse, size = O.attention(wide(q[0]), wide(k).reshape(-1, d)[:n], wide(v).reshape(-1, d)[:n], 1.0)
+    # every value is positive, so an error of the weights is one of the output: the outputs' rounding, logits as elsewhere, 2^-16 for the weights; and float32's own
+    # sums, n additions of which the tensor cores may cut off
+    loose = ROUND[dtype] + 4 * 128 * 2.0 ** -24 * size + 2.0 ** -16 + n / 32 * 2.0 ** -23
+    assert (np.abs(wide(out[0]) - want) <= loose * want + 2.0 ** -25).all(), (np.abs(wide(out[0]) / want - 1).max(), loose)
+    assert np.abs(wide(lse[0]) - want_lse).max() <= 2 * 128 * 2.0 ** -24 * size + 4e-6 * max(1.0, np.abs(want_lse).max())
+
+
+@pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (F16, F16), (BF16, E4M3), (F16, E4M3)])
 @pytest.mark.parametrize("route", ROUTES)
 def test_weights_are_not_rounded(cosa, dtype, cache, route):
     """Two tokens of opposite values, whose logits differ by little: the output is a small difference of the two weights, in which an error of
