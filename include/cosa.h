@@ -449,7 +449,8 @@ int cosa_decode_select_ex(const cosa_cache* cache, const void* q, int32_t batch,
  * cosa_decode_attention -- attention of one new token of each request over its cached tokens (the new one among them).
  *   out[b,h] = sum_t softmax_t(softmax_scale * q[b,h] . k[t]) v[t],  out_lse[b,h] = ln sum_t exp(softmax_scale * q[b,h] . k[t])
  * over t in [max(0, lens[b] - window), lens[b]), and with lists only those in the listed pages.  A row with no such token (or whose
- * logits are all -inf) gets zeros and -inf.  Rows of the pages at and past lens[b] are never used, whatever they hold.
+ * logits are all -inf) gets zeros and -inf.  One with a logit that is NaN or +inf gets NaN, outputs and lse, however the row was divided.  Rows
+ * of the pages at and past lens[b] are never used, whatever they hold.
  *   q          in   [batch, hq, d]; query head h reads KV head h / (hq / hkv)
  *   lens       in   [batch]; more than the table's row holds counts as that much
  *   pages      in   [batch, hkv, list_stride] logical pages in any order, each at most once; NULL: all.  Entries outside the request's

@@ -557,12 +557,15 @@ __global__ void __launch_bounds__(kThreads, 1) decode_attention_kernel(DecodePar
         const float vs = E4M3 ? c.v_scale[kvh] : 1.f;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const float inv0 = l[n][0] > 0.f ? vs / l[n][0] : 0.f, inv1 = l[n][1] > 0.f ? vs / l[n][1] : 0.f;
+          // (a sum of zero: no logit above -inf, and no tokens in effect; one that is no number goes on to the outputs)
+          const bool none0 = l[n][0] == 0.f, none1 = l[n][1] == 0.f;
+          const float inv0 = vs / l[n][0], inv1 = vs / l[n][1];
           const int head = n * 8 + g;
           typename H::T* dst = static_cast<typename H::T*>(p.out) + b * p.out_request + (long long)(head0 + head) * p.out_head;
 #pragma unroll
           for (int j = 0; j < kSteps; ++j) {
-            const typename H::T2 first = H::narrow(o[n][j][0] * inv0, o[n][j][1] * inv1), second = H::narrow(o[n][j][2] * inv0, o[n][j][3] * inv1);
+            const typename H::T2 first = H::narrow(none0 ? 0.f : o[n][j][0] * inv0, none1 ? 0.f : o[n][j][1] * inv1),
+                                 second = H::narrow(none0 ? 0.f : o[n][j][2] * inv0, none1 ? 0.f : o[n][j][3] * inv1);
             const uint32_t x0 = ptx::transpose_8x8(*reinterpret_cast<const uint32_t*>(&first)), x1 = ptx::transpose_8x8(*reinterpret_cast<const uint32_t*>(&second));
             if (head < heads) {
               if constexpr (E4M3) {
@@ -577,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_attention_kernel(DecodePar
 #pragma unroll
             for (int i = 0; i < 2; ++i)
               if (n * 8 + 2 * t4 + i < heads)
-                p.lse[(long long)b * p.hq + head0 + n * 8 + 2 * t4 + i] = l[n][i] > 0.f ? top[n][i] * kLn2 + logf(l[n][i]) : -INFINITY;
+                p.lse[(long long)b * p.hq + head0 + n * 8 + 2 * t4 + i] = l[n][i] == 0.f ? -INFINITY : top[n][i] * kLn2 + logf(l[n][i]);
         }
       } else {
         // piece 1 (begins its row, which goes on) is the run's last: it takes the place of the ring
@@ -668,11 +671,11 @@ __global__ void __launch_bounds__(kThreads, 1) decode_attention_kernel(DecodePar
           for (int i = 0; i < kVec; ++i) sum_o[i] += w * y[piece_at(head, i * 32 + lane)];
         }
         if (whole) {
-          const float inv = sum_l > 0.f ? (E4M3 ? c.v_scale[rh] : 1.f) / sum_l : 0.f;
+          const float inv = (E4M3 ? c.v_scale[rh] : 1.f) / sum_l;
           typename H::T* dst = static_cast<typename H::T*>(p.out) + rb * p.out_request + (long long)(h0 + head) * p.out_head + lane;
 #pragma unroll
-          for (int i = 0; i < kVec; ++i) dst[i * 32] = H::narrow1(sum_o[i] * inv);
-          if (p.lse && lane == 0) p.lse[(long long)rb * p.hq + h0 + head] = sum_l > 0.f ? most * kLn2 + logf(sum_l) : -INFINITY;
+          for (int i = 0; i < kVec; ++i) dst[i * 32] = H::narrow1(sum_l == 0.f ? 0.f : sum_o[i] * inv);
+          if (p.lse && lane == 0) p.lse[(long long)rb * p.hq + h0 + head] = sum_l == 0.f ? -INFINITY : most * kLn2 + logf(sum_l);
         } else {
           float* to = s.parts.data + ((long long)blockIdx.x * 2 + which) * s.slot_heads * (D + 4);
 #pragma unroll

@@ -64,9 +64,9 @@ __global__ void __launch_bounds__(kWarps * 32) decode_check_kernel(DecodeParams 
     for (int i = 0; i < per; ++i) {
       float x = 0.f;
       for (int w = 0; w < kWarps; ++w) x += s_out[w][lane * per + i] * expf(s_top[w] - ref);
-      static_cast<T*>(p.out)[b * p.out_request + hq * p.out_head + lane * per + i] = H::narrow1(sum > 0.f ? x / sum : 0.f);
+      static_cast<T*>(p.out)[b * p.out_request + hq * p.out_head + lane * per + i] = H::narrow1(sum == 0.f ? 0.f : x / sum);
     }
-    if (p.lse && lane == 0) p.lse[(long long)b * p.hq + hq] = sum > 0.f ? ref + logf(sum) : -INFINITY;
+    if (p.lse && lane == 0) p.lse[(long long)b * p.hq + hq] = sum == 0.f ? -INFINITY : ref + logf(sum);
   }
 }
 

@@ -52,18 +52,18 @@ __device__ __forceinline__ void join_head(const DecodeParams& p, const float* da
         const float w = __shfl_sync(0xffffffffu, weight, i1 + i);
 #pragma unroll
         for (int v = 0; v < kVec; ++v) {
-          out[v] = w > 0.f ? fmaf(w, x[i][v], out[v]) : out[v];                   // (a piece of no weight adds nothing, whatever it holds)
+          out[v] = i0 + i1 + i < n ? fmaf(w, x[i][v], out[v]) : out[v];           // (past the last piece the last comes again; one of no weight may hold no number, and says so)
           x[i][v] = next[i][v];
         }
       }
     }
   }
-  const float inv = sum > 0.f ? (p.c.e4m3 ? p.c.v_scale[h] : 1.f) / sum : 0.f;
+  const float inv = (p.c.e4m3 ? p.c.v_scale[h] : 1.f) / sum;                       // (a sum of zero: no tokens in effect; one that is no number goes on to the outputs)
   const int hq = h * p.group + ch * per_chunk + head;
   typename H::T* dst = static_cast<typename H::T*>(p.out) + b * p.out_request + (long long)hq * p.out_head + lane * kVec;
 #pragma unroll
-  for (int v = 0; v < kVec; v += 2) *reinterpret_cast<typename H::T2*>(dst + v) = H::narrow(out[v] * inv, out[v + 1] * inv);
-  if (p.lse && lane == 0) p.lse[(long long)b * p.hq + hq] = sum > 0.f ? most * 0.6931471805599453f + logf(sum) : -INFINITY;
+  for (int v = 0; v < kVec; v += 2) *reinterpret_cast<typename H::T2*>(dst + v) = H::narrow(sum == 0.f ? 0.f : out[v] * inv, sum == 0.f ? 0.f : out[v + 1] * inv);
+  if (p.lse && lane == 0) p.lse[(long long)b * p.hq + hq] = sum == 0.f ? -INFINITY : most * 0.6931471805599453f + logf(sum);
 }
 
 }  // namespace cosa

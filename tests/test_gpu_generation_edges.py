@@ -1,4 +1,5 @@
 """Generation from a paged cache where it is easily wrong: sizes at a limit of the launch, numbers that are not finite, weights far below a row's largest."""
+import math
 import os
 import subprocess
 import sys
@@ -68,6 +69,59 @@ def attend(cosa, q, k, v, ks, vs, table, lens, route):
 
 
 ROUTES = ["as usual", "one CTA", "workspace", "check"]
+
+
+@pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (F16, F16), (BF16, E4M3), (F16, E4M3)])
+@pytest.mark.parametrize("lens", [[40, 3], [20000, 300]])
+@pytest.mark.parametrize("route", ROUTES)
+def test_logits_that_are_not_numbers_make_their_heads_nan(cosa, dtype, cache, lens, route):
+    """NaN or +inf in a query, one key or a whole run of keys: outputs and lse of the heads that meet it are NaN, however the row is divided; all
+    others are those of the call without it, bit by bit."""
+    hq, hkv, d, page, n = 6, 2, 64, 16, lens[0]
+    inputs = contents(lens, hq, hkv, d, page, dtype, cache, seed=n + d)
+    q, k, v, ks, vs, table = inputs
+    q[0, :, 3] = q[0, :, 3].abs() + 0.25
+    right = attend(cosa, *inputs, lens, route)
+    assert all(bool(torch.isfinite(x).all()) for x in right)
+
+    def check(q, k, poisoned):
+        out, lse = attend(cosa, q, k, v, ks, vs, table, lens, route)
+        bad = torch.zeros(len(lens), hq, dtype=torch.bool, device="cuda")
+        bad[0, poisoned] = True
+        assert bool(out[bad].isnan().all()) and bool(lse[bad].isnan().all()), (out[bad], lse[bad])
+        assert torch.equal(out[~bad], right[0][~bad]) and torch.equal(lse[~bad], right[1][~bad])
+
+    for x in (math.nan, math.inf):
+        other = q.clone()
+        other[0, 4, 3] = x
+        check(other, k, [4])
+    some = range(n // 3, n // 3 + max(1, n // 2))
+    for x, tokens in ((math.nan, [n - 1]), (math.nan, [0]), (math.nan, some), (math.nan, range(n)), (math.inf, [n // 2]), (math.inf, some)):
+        if x == math.inf and cache is E4M3:
+            continue      # (e4m3 has none)
+        other = k.clone()
+        put(other, table, page, 0, 1, tokens, 3, x)
+        check(q, other, [3, 4, 5])
+
+
+@pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (F16, F16)])
+@pytest.mark.parametrize("n", [40, 20000])
+@pytest.mark.parametrize("route", ROUTES)
+def test_logits_of_minus_infinity(cosa, dtype, cache, n, route):
+    """Keys of -inf where the queries are positive: left out; a row that has no other is one without tokens."""
+    hq, hkv, d, page = 4, 2, 64, 16
+    q, k, v, ks, vs, table = contents([n], hq, hkv, d, page, dtype, cache, seed=n)
+    q[0, :, 3] = q[0, :, 3].abs() + 0.25
+    put(k, table, page, 0, 0, range(n), 3, -math.inf)
+    put(k, table, page, 0, 1, range(n - 5), 3, -math.inf)
+    out, lse = attend(cosa, q, k, v, ks, vs, table, [n], route)
+    assert bool((out[0, :2] == 0).all()) and bool(torch.isneginf(lse[0, :2]).all())
+    t = np.arange(n - 5, n)
+    at, off = table[0][t // page], t % page
+    want, want_lse, size = O.attention(wide(q[0, 2:]), wide(k)[at, 1, off], wide(v)[at, 1, off], d ** -0.5)
+    top = np.abs(wide(v)[at, 1, off]).max()
+    assert (np.abs(wide(out[0, 2:]) - want) <= ROUND[dtype] * np.abs(want) + (4 * 128 * 2.0 ** -24 * size + 2.0 ** -16) * top).all()
+    assert np.abs(wide(lse[0, 2:]) - want_lse).max() <= 2 * 128 * 2.0 ** -24 * size + 4e-6 * max(1.0, np.abs(want_lse).max())
 
 
 @pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (F16, F16), (BF16, E4M3), (F16, E4M3)])
