@@ -428,7 +428,8 @@ int cosa_cache_append_ex(const cosa_cache* cache, const void* k_new, const void*
 /*
  * cosa_decode_select -- the pages a new token of each request attends to, one list per KV head.
  * For query head g of the group and page j:  M[g,j] = sum_c max(q_c low_jc, q_c high_jc), an upper bound of q . k over the page's keys.
- * A page's rank is r[j] = max_g (M[g,j] - max_j' M[g,j']): 0 where it holds the maximum of a head, below elsewhere.  Kept are the first
+ * A page's rank is r[j] = max_g (M[g,j] - max_j' M[g,j']): 0 where it holds the maximum of a head (be it +inf), below elsewhere.  Of two products
+ * of which one is NaN (zero times an infinite bound) the other counts; a score that is NaN, and a head whose scores are all -inf, count for nothing.  Kept are the first
  * keep_first and last keep_last pages, then those of largest r, equal ones by index, until
  *     K = min(n, max(cosa_budget_count(budget, n), min_pages, keep_first + keep_last))
  * of the request's n = ceil(lens / page_size) pages are.

@@ -72,9 +72,11 @@ def budget_pages(budget, n, least=1, first=0, last=0):
 
 
 def page_scores(q, low, high):
-    """M [G, n]: sum_c max(q_c low_c, q_c high_c) in float32, by the tree of the definition.  q [G,d], low and high [n,d] float32."""
+    """M [G, n]: sum_c max(q_c low_c, q_c high_c) in float32, by the tree of the definition; of two products of which one is no number (zero times
+    infinity) the other.  q [G,d], low and high [n,d] float32."""
     q, low, high = (np.asarray(x, np.float32) for x in (q, low, high))
-    x = np.maximum(q[:, None] * low[None], q[:, None] * high[None]).reshape(q.shape[0], low.shape[0], -1, 8)
+    with np.errstate(invalid="ignore"):
+        x = np.fmax(q[:, None] * low[None], q[:, None] * high[None]).reshape(q.shape[0], low.shape[0], -1, 8)
     while x.shape[3] > 1:
         half = x.shape[3] // 2
         x = x[..., :half] + x[..., half:]
@@ -86,12 +88,16 @@ def page_scores(q, low, high):
 
 
 def select(q, low, high, budget, least=1, first=0, last=0):
-    """Ascending list of the pages kept, of n; q [G,d]."""
+    """Ascending list of the pages kept, of n; q [G,d].  A page that holds a head's maximum ranks 0 for it, whatever that maximum is; a score that is no
+    number counts for nothing."""
     n = low.shape[0]
     if n == 0:
         return np.zeros(0, np.int64)
     m = page_scores(q, low, high)
-    r = (m - m.max(axis=1, keepdims=True)).max(axis=0).astype(np.float64)
+    m = np.where(np.isnan(m), np.float32(-math.inf), m)
+    top = m.max(axis=1, keepdims=True)
+    with np.errstate(invalid="ignore"):
+        r = np.where((m == top) & (m > -math.inf), np.float32(0), np.where(m == -math.inf, m, m - top)).max(axis=0).astype(np.float64)
     r[:first] = math.inf
     r[n - min(n, last):] = math.inf
     order = sorted(range(n), key=lambda j: (-r[j], j))

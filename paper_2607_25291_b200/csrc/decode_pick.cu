@@ -112,6 +112,12 @@ __global__ void __launch_bounds__(kThreads) decode_pick_kernel(SelectParams p, b
     __syncthreads();
     const float4 others = *reinterpret_cast<const float4*>(tops[lane % kWarps]);
     top[0] = ptx::warp_max(others.x); top[1] = ptx::warp_max(others.y); top[2] = ptx::warp_max(others.z); top[3] = ptx::warp_max(others.w);
+    // A page that holds the maximum ranks 0 whatever that maximum is (inf - inf would be no number, and be passed over); a head without a score above -inf has
+    // none: NaN equals nothing and gives no ranks
+#pragma unroll
+    for (int g = 0; g < kHeadsAtOnce; ++g)
+      if (top[g] == -INFINITY) top[g] = NAN;
+    auto rank = [](float x, float top) { return x == top ? 0.f : __fsub_rn(x, top); };
     const bool begin = g0 == 0, end = g0 + kHeadsAtOnce >= p.group;
     float* so_far = reinterpret_cast<float*>(keys);                               // (until they are whole the ranks lie where the keys will)
     for (int i = tid; i < quads; i += kThreads) {
@@ -120,8 +126,8 @@ __global__ void __launch_bounds__(kThreads) decode_pick_kernel(SelectParams p, b
       for (int g = 0; g < kHeadsAtOnce; ++g)
         if (g0 + g < p.group) {
           const float4 x = *reinterpret_cast<const float4*>(mg + (long long)g * m_pitch + i * 4);
-          r.x = fmaxf(r.x, __fsub_rn(x.x, top[g])); r.y = fmaxf(r.y, __fsub_rn(x.y, top[g]));
-          r.z = fmaxf(r.z, __fsub_rn(x.z, top[g])); r.w = fmaxf(r.w, __fsub_rn(x.w, top[g]));
+          r.x = fmaxf(r.x, rank(x.x, top[g])); r.y = fmaxf(r.y, rank(x.y, top[g]));
+          r.z = fmaxf(r.z, rank(x.z, top[g])); r.w = fmaxf(r.w, rank(x.w, top[g]));
         }
       if (!end) {
         *reinterpret_cast<float4*>(so_far + i * 4) = r;

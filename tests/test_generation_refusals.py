@@ -196,3 +196,20 @@ def test_expanded_tensors_of_a_prompt_are_refused(B, monkeypatch):
         if slot < 2:
             with pytest.raises(ValueError):
                 B.cosa_kap_select(args[0], args[1], 0.5, *lists)
+
+
+def test_oracle_of_infinite_scores_by_hand():
+    """A page of infinite score holds its head's maximum; a head that knows only -inf, and a score that is no number, have no say."""
+    inf, q = np.inf, np.array([[1.0, 0.0] + [0.0] * 62, [0.0, -1.0] + [0.0] * 62])
+    low, high = np.zeros((4, 64)), np.zeros((4, 64))
+    low[:, 0], high[:, 0] = -1.0, [1.0, 2.0, inf, 3.0]
+    low[:, 1], high[:, 1] = [-5.0, -1.0, -1.0, -2.0], 0.0
+    assert O.page_scores(q, low, high).tolist() == [[1.0, 2.0, inf, 3.0], [5.0, 1.0, 1.0, 2.0]]
+    assert O.select(q, low, high, 0.25).tolist() == [0] and O.select(q, low, high, 0.5).tolist() == [0, 2] and O.select(q, low, high, 0.75).tolist() == [0, 2, 3]
+    q[1, 0] = 0.5
+    low[:, 0], high[:, 0] = [-1.0, -1.0, -inf, -1.0], [-1.0, -1.0, -inf, -1.0]
+    assert O.select(q, low, high, 0.5).tolist() == [0, 1]      # the first head has its maximum in pages 0, 1 and 3, the second in page 0
+    low[:, 0], high[:, 0] = -inf, -inf
+    assert O.select(q, low, high, 0.5).tolist() == [0, 1]      # nobody has a say: the lowest indices
+    low[0, 0], high[0, 0] = inf, -inf      # (the bounds of a page whose keys are all NaN in this channel)
+    assert O.page_scores(q, low, high)[0].tolist() == [inf, -inf, -inf, -inf]

@@ -168,3 +168,34 @@ def test_weights_are_not_rounded(cosa, dtype, cache, route):
     # (the bound for two 16-bit terms, with values of 1)
     bad = np.abs(wide(out[0]) - want) - (ROUND[dtype] * np.abs(want) + 4 * 128 * 2.0 ** -24 * size + 2.0 ** -16 + 2.0 ** -25)
     assert bad.max() <= 0, float(bad.max())
+
+
+# ---------------------------------------------------------------- selection
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("pages", [[30], [3, 40, 41], [69], list(range(1, 70, 2)), list(range(70))])
+@pytest.mark.parametrize("leaning", ["all", "one head", "none"])
+def test_select_of_pages_with_infinite_scores(cosa, dtype, pages, leaning):
+    """A page whose score is +inf holds that head's maximum and comes first, and of several the lowest indices; the other heads rank as ever."""
+    page, n, hq, hkv, d = 16, 70, 6, 2, 128
+    torch.manual_seed(len(pages))
+    low = -torch.rand(n, hkv, d, device="cuda") - 0.1
+    high = -low * torch.rand(n, hkv, d, device="cuda")
+    high[pages, :, 5] = math.inf
+    bounds = torch.stack([low, high], dim=2).to(dtype).contiguous()
+    q = torch.randn(1, hq, d, device="cuda")
+    towards = q[0, :, 5].abs() + 0.1
+    q[0, :, 5] = towards if leaning == "all" else -towards
+    if leaning == "one head":
+        q[0, 1::3, 5] = towards[1::3]
+    q = q.to(dtype)
+    got, count = torch.empty(1, hkv, 12, dtype=torch.int32, device="cuda"), torch.empty(1, hkv, dtype=torch.int32, device="cuda")
+    handle = cosa.make_cache(None, None, gpu([range(n)]), bounds=bounds, page_size=page)
+    cosa.cosa_decode_select(handle, q, gpu([n * page]), 0.15, got, count)
+    qs, bs = q.float().cpu().numpy(), bounds.float().cpu().numpy()
+    for h in range(hkv):
+        want = O.select(qs[0, h * 3:h * 3 + 3], bs[:, h, 0], bs[:, h, 1], 0.15)
+        kept = got[0, h, :int(count[0, h])].tolist()
+        assert kept == want.tolist() and len(kept) == 11
+        if leaning != "none":
+            # (beside them no more than a page of each other head's maximum, which ranks 0 as well)
+            assert sum(j in pages for j in kept) >= min(len(pages), len(kept) - (0 if leaning == "all" else 2))
