@@ -771,7 +771,7 @@ cudaError_t launch_decode_attention(const DecodeParams& p, cudaStream_t st) {
   s.slot_heads = std::min(p.group, per_chunk);
   // no more CTAs than the longest rows that the tables allow could use
   long long row_tokens = p.pages ? (long long)p.list_stride << c.page_shift : (long long)c.table_stride << c.page_shift;
-  if (p.window > 0 && !p.pages) row_tokens = std::min<long long>(row_tokens, p.window + tile_rows);
+  if (p.window > 0 && !p.pages) row_tokens = std::min<long long>(row_tokens, (long long)p.window + tile_rows);
   const long long row_tiles = (row_tokens + tile_rows - 1) / tile_rows;
   const long long useful = (row_tiles * s.units * s.per_unit / kMinTiles + kWarps - 1) / kWarps;
   const int ctas = p.ctas > 0 ? std::min(p.ctas, sms) : sms;

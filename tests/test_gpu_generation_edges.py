@@ -170,6 +170,20 @@ def test_weights_are_not_rounded(cosa, dtype, cache, route):
     assert bad.max() <= 0, float(bad.max())
 
 
+@pytest.mark.parametrize("lens,hq,hkv,page", [([20000], 8, 2, 16), ([5000, 0, 1, 900], 32, 8, 64)])
+def test_windows_of_any_size(cosa, lens, hq, hkv, page):
+    """A window that no request fills is none: the same division of the work, the same bits."""
+    q, k, v, _, _, table = contents(lens, hq, hkv, 128, page, BF16, BF16, seed=2)
+    handle = cosa.make_cache(k, v, gpu(table))
+    results = []
+    for window in (0, 2 ** 31 - 1, 2 ** 31 - 9, 2 ** 30):
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+        cosa.cosa_decode_attention(handle, q, gpu(lens), out, lse, window=window)
+        results.append((out, lse))
+    for out, lse in results[1:]:
+        assert torch.equal(out, results[0][0]) and torch.equal(lse, results[0][1])
+
+
 # ---------------------------------------------------------------- selection
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("pages", [[30], [3, 40, 41], [69], list(range(1, 70, 2)), list(range(70))])
