@@ -14,7 +14,9 @@ struct NvtxRange {
 };
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// (a kernel that meets a misaligned word faults)
+template <typename... T>
+bool whole_words(const T*... p) { return (((reinterpret_cast<uintptr_t>(p) & (sizeof(T) - 1)) == 0) && ...); }
 bool power_of_two(int x) { return x > 0 && (x & (x - 1)) == 0; }
 int log2_of(int x) {
   int s = 0;
@@ -45,6 +47,7 @@ int view_of(const cosa_cache* c, bool pools, CacheView* v) {
     if (v->e4m3 && (!c->k_scale || !c->v_scale)) return COSA_ERR_INVALID_ARG;
   }
   if (c->k_bounds && !aligned16(c->k_bounds)) return COSA_ERR_INVALID_ARG;
+  if (!whole_words(c->page_table, c->k_scale, c->v_scale)) return COSA_ERR_INVALID_ARG;
   v->k = c->k; v->v = c->v; v->bounds = c->k_bounds;
   v->table = c->page_table; v->k_scale = c->k_scale; v->v_scale = c->v_scale;
   v->table_stride = c->table_stride; v->num_pages = c->num_pages;
@@ -88,7 +91,7 @@ int scratch_for(const cosa_decode_options& o, size_t need, void** out) {
 }
 
 int check_queries(const CacheView& c, const void* q, int batch, int hq, const int32_t* lens) {
-  if (!q || !lens || !c.table || !aligned16(q)) return COSA_ERR_INVALID_ARG;
+  if (!q || !lens || !c.table || !aligned16(q) || !whole_words(lens)) return COSA_ERR_INVALID_ARG;
   if (batch < 1 || hq < 1 || hq % c.hkv != 0) return COSA_ERR_INVALID_ARG;
   if (batch > 65535 || (long long)batch * hq > 0x7fffffffLL) return COSA_ERR_UNSUPPORTED;
   return COSA_OK;
@@ -135,6 +138,7 @@ int cosa_page_plan(const int32_t* lens, const int32_t* grow, int32_t batch, int3
   NvtxRange range("cosa_page_plan");
   if (!lens || !grow || !page_table || !free_ring || !ring_state || !out_lens || !out_ring_state || !out_starts) return COSA_ERR_INVALID_ARG;
   if (batch < 1 || max_tokens < 0 || (max_tokens > 0 && !out_slots)) return COSA_ERR_INVALID_ARG;
+  if (!whole_words(lens, grow, page_table, free_ring, ring_state, out_lens, out_ring_state, out_starts, out_slots, out_positions, out_requests)) return COSA_ERR_INVALID_ARG;
   if (out_lens == lens || out_lens == grow || out_starts == lens || out_starts == grow || out_ring_state == ring_state) return COSA_ERR_INVALID_ARG;
   int rc = check_pages(page_size, num_pages, table_stride);
   if (rc != COSA_OK) return rc;
@@ -158,7 +162,7 @@ int cosa_cache_append_ex(const cosa_cache* cache, const void* k_new, const void*
   if (rc != COSA_OK) return rc;
   if (tokens < 0) return COSA_ERR_INVALID_ARG;
   if (tokens == 0) return COSA_OK;
-  if (!k_new || !v_new || !slots || !aligned16(k_new) || !aligned16(v_new) || !aligned4(slots)) return COSA_ERR_INVALID_ARG;
+  if (!k_new || !v_new || !slots || !aligned16(k_new) || !aligned16(v_new) || !whole_words(slots)) return COSA_ERR_INVALID_ARG;
   const cosa_decode_options o = options_of(opt);
   rc = strides2(o.new_strides, p.c.hkv, p.c.d, tokens > 1, &p.new_token, &p.new_head);
   if (rc != COSA_OK) return rc;
@@ -178,7 +182,7 @@ int cosa_decode_select_ex(const cosa_cache* cache, const void* q, int32_t batch,
   int rc = view_of(cache, false, &p.c);
   if (rc == COSA_OK) rc = check_queries(p.c, q, batch, hq, lens);
   if (rc != COSA_OK) return rc;
-  if (!p.c.bounds || !out_pages || !out_count) return COSA_ERR_INVALID_ARG;
+  if (!p.c.bounds || !out_pages || !out_count || !whole_words(out_pages, out_count)) return COSA_ERR_INVALID_ARG;
   if (!(budget > 0.f) || budget > 1.f) return COSA_ERR_INVALID_ARG;
   const cosa_decode_options o = options_of(opt);
   if (o.min_pages < 0 || o.keep_first < 0 || o.keep_last < 0) return COSA_ERR_INVALID_ARG;
@@ -211,7 +215,7 @@ int cosa_decode_attention_ex(const cosa_cache* cache, const void* q, int32_t bat
   int rc = view_of(cache, true, &p.c);
   if (rc == COSA_OK) rc = check_queries(p.c, q, batch, hq, lens);
   if (rc != COSA_OK) return rc;
-  if (!out || !aligned16(out) || (pages && (!count || list_stride < 1))) return COSA_ERR_INVALID_ARG;
+  if (!out || !aligned16(out) || (pages && (!count || list_stride < 1)) || !whole_words(pages, count, out_lse)) return COSA_ERR_INVALID_ARG;
   const cosa_decode_options o = options_of(opt);
   if (o.window < 0 || o.ctas < 0 || !(o.softmax_scale >= 0.f)) return COSA_ERR_INVALID_ARG;
   if (o.impl != 0 && o.impl != 1) return COSA_ERR_UNSUPPORTED;

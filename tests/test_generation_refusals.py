@@ -213,3 +213,23 @@ def test_oracle_of_infinite_scores_by_hand():
     assert O.select(q, low, high, 0.5).tolist() == [0, 1]      # nobody has a say: the lowest indices
     low[0, 0], high[0, 0] = inf, -inf      # (the bounds of a page whose keys are all NaN in this channel)
     assert O.page_scores(q, low, high)[0].tolist() == [inf, -inf, -inf, -inf]
+
+
+def test_misaligned_words(B):
+    """Pointers to 32- and 64-bit words that are no multiples of their size."""
+    L, off, q = B.library(), ctypes.c_void_p(258), ctypes.c_void_p(4096)
+    for bad in ({"page_table": 258}, {"k_scale": 257, "cache_dtype": B.COSA_E4M3}, {"v_scale": 258, "cache_dtype": B.COSA_E4M3}):
+        c = ctypes.byref(cache(B, **bad))
+        assert L.cosa_cache_append(c, ONE, ONE, ONE, 1, None) == -1
+        assert L.cosa_decode_attention(c, ONE, 1, 8, ONE, None, None, 0, ONE, None, None) == -1
+    c = ctypes.byref(cache(B))
+    for at in range(4):
+        lens, pages, count, lse = (off if i == at else ONE for i in range(4))
+        assert L.cosa_decode_attention(c, ONE, 1, 8, lens, pages, count, 4, ONE, lse, None) == -1
+        if at < 3:
+            assert L.cosa_decode_select(c, ONE, 1, 8, lens, 0.5, pages, count, 10, None) == -1
+    good = [256, 512, 4, 16, 1024, 8, 2048, 50, 4096, 5120, 6144, 7168, 8192, 9216, 10240, 9]
+    for i in (0, 1, 4, 6, 8, 9, 10, 11, 12, 13, 14):
+        for step in ((2, 4) if i in (8, 10) else (1, 2)):
+            args = [x + step if j == i else x for j, x in enumerate(good)]
+            assert L.cosa_page_plan(*(ctypes.c_void_p(x) if x > 200 else x for x in args), None) == -1, i
