@@ -247,7 +247,8 @@ def cosa_workspace_bytes(op: int, shape: CosaShape, opt: CosaOptions | None = No
 def cosa_kap_select(q, k, budget: float, out_order, out_count, causal=True, stream=None, opt: CosaOptions | None = None,
                     block_q: int = 128):
     """Stage 1: fills out_order [B,Hq,nQB,order_stride] / out_count [B,Hq,nQB] (int32); block_q = 256 makes one ranking
-    per 256-row query block (the lists stay per 128-row tile, see cosa.h)."""
+    per 256-row query block (the lists stay per 128-row tile, see cosa.h).  With opt.kv_page_table k is a page pool
+    [P,Hkv,page,d], a cache's own (Cache.tensors) for instance."""
     lib = _lib or _load()
     shape = make_shape(q, k, causal)
     if block_q != 128:
@@ -290,7 +291,8 @@ def cosa_kap_select_static(q, k, budget: float, out_order, out_count, causal=Tru
 
 def cosa_osk_attention(q, k, v, order, count, tightened_budget: float, out, out_lse=None, out_visited=None,
                        causal=True, stream=None, opt: CosaOptions | None = None):
-    """Stage 2: fills out [B,Hq,N,d] bf16, out_lse [B,Hq,N] f32, out_visited [B,Hq,nQB] int32."""
+    """Stage 2: fills out [B,Hq,N,d] bf16, out_lse [B,Hq,N] f32, out_visited [B,Hq,nQB] int32.  With opt.kv_page_table k and v
+    are page pools, as in cosa_kap_select."""
     lib = _lib or _load()
     shape = make_shape(q, k, causal)
     (qp, qstr), (op, ostr) = _strided_ptr(q, "q"), _strided_ptr(out, "out")

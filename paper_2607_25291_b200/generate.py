@@ -70,14 +70,12 @@ class Stack:
             cosa.cosa_cache_append(cache, k[real], v[real], slots)
             opt = cosa.default_options(order_stride=order.shape[-1], seq_lens=lens, skip_scale=0.3 * min(self.prompts))
             heads = lambda t: t.transpose(1, 2)  # noqa: E731
+            ks, vs = heads(k), heads(v)
             if dense:      # straight from the pages (an 8-bit cache serves the tokens after the prompt)
                 opt.kv_page_table, opt.kv_page_size, opt.kv_num_pages = table.data_ptr(), self.page, cache.num_pages
-                ks, vs = cache.tensors[0], cache.tensors[1]
-                shape_k = torch.empty(self.batch, self.hkv, n, 0, device=dev)      # (only its shape is read)
-                _prefill_paged(heads(q), ks, vs, shape_k, budget, tightened, order, count, heads(out), opt)
-            else:
-                cosa.cosa_kap_select(heads(q), heads(k), budget, order, count, opt=opt)
-                cosa.cosa_osk_attention(heads(q), heads(k), heads(v), order, count, tightened, heads(out), opt=opt)
+                ks, vs = cache.tensors[:2]
+            cosa.cosa_kap_select(heads(q), ks, budget, order, count, opt=opt)
+            cosa.cosa_osk_attention(heads(q), ks, vs, order, count, tightened, heads(out), opt=opt)
             x = x + out.flatten(2) @ self.w_out[i]
         return x[torch.arange(self.batch, device=dev), lens.long() - 1]
 
@@ -102,20 +100,6 @@ class Stack:
         most = max(cosa.cosa_budget_count(budget, self.table.shape[1]), 2)
         return (torch.empty(self.batch, self.hkv, most, dtype=torch.int32, device="cuda"),
                 torch.empty(self.batch, self.hkv, dtype=torch.int32, device="cuda"))
-
-
-def _prefill_paged(q, ks, vs, k_shape, budget, tightened, order, count, out, opt):
-    """KAP and OSK over page pools through the C calls: the shape comes from the batch, not from the pools."""
-    from ctypes import byref
-    lib, shape = cosa.library(), cosa.make_shape(q, k_shape)
-    opt.q_strides[:] = q.stride()[:3]
-    opt.out_strides[:] = out.stride()[:3]
-    stream = cosa._stream_ptr(None)
-    for rc in (lib.cosa_kap_select_ex(q.data_ptr(), ks.data_ptr(), byref(shape), budget, order.data_ptr(), count.data_ptr(), stream, byref(opt)),
-               lib.cosa_osk_attention_ex(q.data_ptr(), ks.data_ptr(), vs.data_ptr(), byref(shape), order.data_ptr(), count.data_ptr(), tightened,
-                                         out.data_ptr(), 0, 0, stream, byref(opt))):
-        if rc:
-            raise cosa.CosaError(rc, "prefill")
 
 
 def step_time(stack: Stack, x, budget: float, tokens: int) -> float:

@@ -233,3 +233,11 @@ def test_misaligned_words(B):
         for step in ((2, 4) if i in (8, 10) else (1, 2)):
             args = [x + step if j == i else x for j, x in enumerate(good)]
             assert L.cosa_page_plan(*(ctypes.c_void_p(x) if x > 200 else x for x in args), None) == -1, i
+
+
+def test_the_example_uses_what_a_user_has():
+    """Its prompt goes from the cache's pools through the binding's public calls."""
+    import inspect
+    import re
+    from paper_2607_25291_b200 import generate
+    assert not re.search(r"cosa\._|library\(|byref", inspect.getsource(generate))
