@@ -138,6 +138,12 @@ def main():
     p.add_argument("--e4m3", action="store_true", help="8-bit cache")
     a = p.parse_args()
     prompts = [int(n) for n in a.prompts.split(",")]
+    if min(prompts) < 1 or any(n % 128 for n in prompts):
+        p.error("prompts have to be multiples of 128")
+    if a.page < 8 or a.page & (a.page - 1) or max(prompts) % a.page:
+        p.error("the page size has to be a power of two from 8 on that divides the longest prompt")
+    if a.tokens < 2 or not 0 < a.budget <= 1:
+        p.error("at least two tokens, and a budget in (0, 1]")
     torch.cuda.set_device(0)
     for budget in dict.fromkeys((a.budget, 1.0)):
         stack = Stack(prompts, a.tokens + 8, layers=a.layers, page=a.page, e4m3=a.e4m3)

@@ -241,3 +241,13 @@ def test_the_example_uses_what_a_user_has():
     import re
     from paper_2607_25291_b200 import generate
     assert not re.search(r"cosa\._|library\(|byref", inspect.getsource(generate))
+
+
+@pytest.mark.parametrize("args", [["--tokens", "1"], ["--prompts", "200"], ["--prompts", "256,0"], ["--page", "48"], ["--page", "256", "--prompts", "384"],
+                                  ["--budget", "0"], ["--budget", "1.5"]])
+def test_the_example_refuses(args, monkeypatch, capsys):
+    from paper_2607_25291_b200 import generate
+    monkeypatch.setattr("sys.argv", ["generate", *args])
+    with pytest.raises(SystemExit) as e:
+        generate.main()
+    assert e.value.code == 2 and "error" in capsys.readouterr().err
