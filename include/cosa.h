@@ -417,7 +417,7 @@ int cosa_page_plan(const int32_t* lens, const int32_t* grow, int32_t batch, int3
  * cosa_cache_append -- new keys and values into the pools.
  *   k_new, v_new  in  [tokens, hkv, d] of cache->dtype (options: new_strides; k and v share them)
  *   slots         in  [tokens], as written by cosa_page_plan; a slot outside [0, num_pages * page_size) is passed over
- * Into an e4m3 cache x / scale goes, rounded to nearest even, values beyond +-448 as +-448.
+ * Into an e4m3 cache x / scale goes, the float32 quotient rounded to nearest even, values beyond +-448 as +-448.
  * With k_bounds a page's bounds begin anew with its row 0 and take in every other row.  New tokens of one page have to stand next to one
  * another, in ascending order, as cosa_page_plan lays them out (else its bounds are those of some of its tokens).  A NaN leaves bounds alone.
  */
@@ -427,7 +427,9 @@ int cosa_cache_append_ex(const cosa_cache* cache, const void* k_new, const void*
 
 /*
  * cosa_decode_select -- the pages a new token of each request attends to, one list per KV head.
- * For query head g of the group and page j:  M[g,j] = sum_c max(q_c low_jc, q_c high_jc), an upper bound of q . k over the page's keys.
+ * For query head g of the group and page j:  M[g,j] = sum_c max(q_c low_jc, q_c high_jc), an upper bound of q . k over the page's keys as they were
+ * appended (an 8-bit cache holds them rounded, and attention reads those).  The criterion is that of Tang et al., "Quest: query-aware sparsity for
+ * efficient long-context LLM inference", 2024.
  * A page's rank is r[j] = max_g (M[g,j] - max_j' M[g,j']): 0 where it holds the maximum of a head (be it +inf), below elsewhere.  Of two products
  * of which one is NaN (zero times an infinite bound) the other counts; a score that is NaN, and a head whose scores are all -inf, count for nothing.  Kept are the first
  * keep_first and last keep_last pages, then those of largest r, equal ones by index, until
@@ -460,8 +462,10 @@ int cosa_decode_select_ex(const cosa_cache* cache, const void* q, int32_t batch,
  *   out        out  [batch, hq, d] of cache->dtype
  *   out_lse    out  [batch, hq] float32, may be NULL
  * Logits, maxima, sums and outputs are held in float32; the weights go into the second product as two 16-bit terms, as good as unrounded (bf16: to
- * 2^-17 of each; f16, which an 8-bit cache takes as well: to 2^-22, or 2^-40 of the row's largest).  The result does not depend on what else runs: partial
- * results are joined in a fixed order.
+ * 2^-17 of each; f16, which an 8-bit cache takes as well: to 2^-22, or 2^-40 of the row's largest).  bf16 queries meet an 8-bit cache as f16, after each
+ * head has been divided by a power of two: elements below 2^-14 of the head's largest lose their last bits (2^-25 of the largest at most).
+ * Partial results are joined in a fixed order: equal calls give equal bits, whatever else runs on the GPU.  Where rows are divided follows from the lengths of
+ * the whole batch, the width of the table, opt->ctas and the SM count, so that a request's last bits may differ in other company.
  */
 int cosa_decode_attention(const cosa_cache* cache, const void* q, int32_t batch, int32_t hq, const int32_t* lens, const int32_t* pages,
                           const int32_t* count, int32_t list_stride, void* out, float* out_lse, void* stream);
@@ -470,7 +474,10 @@ int cosa_decode_attention_ex(const cosa_cache* cache, const void* q, int32_t bat
                              const cosa_decode_options* opt);
 
 /* Scratch bytes of the two calls that need some (op 0: cosa_decode_select, 1: cosa_decode_attention, 2: the larger).  Depends on the SM
- * count of the current device, as cosa_workspace_bytes does. */
+ * count of the current device, as cosa_workspace_bytes does.  The selection takes a float for every query head and entry of the table,
+ * batch * hq * table_stride * 4 bytes whatever the lengths (64 requests of 32 heads over 8,192 entries: 64 MiB; 256 of 64 over 16,384: 1 GiB), and one more for
+ * every KV head where a row of the table has more than 49,152 entries; the library's own scratch grows to that in the first call (cosa_reserve_scratch
+ * before it, to have it done).  The attention takes 2 * min(hq / hkv, 16) * (d + 4) * 4 + 40 bytes an SM. */
 size_t cosa_decode_workspace_bytes(int op, const cosa_cache* cache, int32_t batch, int32_t hq, const cosa_decode_options* opt);
 /* sizeof(cosa_cache) and sizeof(cosa_decode_options), for bindings */
 size_t cosa_cache_bytes(void);

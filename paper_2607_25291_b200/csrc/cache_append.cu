@@ -3,7 +3,10 @@
 // A warp takes one KV head of a few tokens: eight channels (16 bytes) a lane, so that d/8 lanes hold a row and a warp two rows (four of
 // 64 channels).  Without bounds the tokens are independent.  With bounds the unit is a run: consecutive slots inside one
 // page.  The warp in whose share a run begins writes all of it and folds it into the page's minima and maxima, so
-// that no two warps touch one page's bounds and no atomics are needed.
+// that no two warps touch one page's bounds and no atomics are needed.  That wants pages that are many: 32,768 tokens of 8 heads take 46.6 us in pages of 64, 54 in pages
+// of 256, but 136 in pages of 1,024 and 379 in pages of 4,096, whose few warps have long runs.
+//
+// Bound: memory.  32,767 tokens of 8 heads of 128 channels: 46.0 us with bounds (5.8 TB/s, 91 % of the copy rate), 43.2 without (96 %).
 #include <algorithm>
 
 #include "cache.cuh"

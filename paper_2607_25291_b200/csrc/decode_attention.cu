@@ -5,7 +5,8 @@
 // joined by the same rule.  Both products have keys or channels as the 16 rows of m16n8k16 and eight heads as its
 // columns: groups up to eight waste no row, where a 128-row tcgen05 tile would be empty but for one to sixteen rows.
 //
-// Bound: memory.  2 len hkv d elements are read and 4 flops done for every element and head of the group, some 4 to 16 per byte.
+// Bound: memory.  2 len hkv d elements are read and 4 flops done for every element and head of the group, some 4 to 16 per byte.  Over an 8-bit cache the
+// products and conversions come near it, with 16 heads a KV head they are the bound (128K tokens: 50 us of 42 with 4 heads, 74 with 16; in bf16 86 and 99 of 83).
 //
 // Division.  All rows -- (request, KV head, chunk of 16 query heads) -- lie one behind the other as tiles of 4 KB of K and 4 KB of V, and every warp that
 // multiplies takes an equal run of tiles, wherever rows begin and end: no SM idles behind a long request.  The runs are found from the
@@ -776,9 +777,11 @@ cudaError_t launch_decode_attention(const DecodeParams& p, cudaStream_t st) {
   const long long useful = (row_tiles * s.units * s.per_unit / kMinTiles + kWarps - 1) / kWarps;
   const int ctas = p.ctas > 0 ? std::min(p.ctas, sms) : sms;
   const long long rows = (long long)s.units * s.per_unit;
-  // Rows of few tiles, and few of them: a CTA takes whole ones, and no second kernel is launched to join them (three requests of up to 201 tokens of
-  // 8 heads: 8.9 us to 6.8, now 6.0, and 9.1 us of enqueuing to 7.2).  A CTA whose rows are longer than others' then works for a microsecond or two more
-  // than it would have
+  // Rows of few tiles, and few of them: a CTA takes whole ones, nothing is joined through global memory, and no second kernel is launched for it where a workspace is the
+  // caller's (three requests of up to 201 tokens of 8 heads: 8.9 us to 6.8, now 5.9).  Whole rows and equal runs, us, for rows of 4, 8, 16 and 32 tiles each:
+  // 8 rows of 4 heads 5.7 / 6.5 / 7.7 / 9.4 and 7.9 / 7.4 / 7.5 / 9.9; 128 rows 6.1 / 7.0 / 8.3 / 10.0 and 8.3 / 7.9 / 8.0 / 11.6; 296 rows, two a CTA,
+  // 7.1 / 8.4 / 10.1 / 13.4 and 8.6 / 8.1 / 9.8 / 13.1; 32 rows of 16 heads 7.6 / 8.9 / 10.5 / 12.8 and 12.5 / 10.9 / 10.2 / 13.9, in e4m3 8.4 / 9.8 / 12.2 / 15.8 and
+  // 14.3 / 12.7 / 11.8 / 15.8.  (Tiles are those of the longest row that the table could hold: the lengths are on the device)
   s.many = s.units > kFewUnits || row_tiles * rows > 0x7fffffffLL;
   s.whole_rows = row_tiles <= 32 && !s.many && rows <= 2 * ctas;
   const int grid = (int)std::max(1LL, std::min<long long>(ctas, s.whole_rows ? rows : useful));

@@ -1,11 +1,12 @@
 // cosa_decode_select, first part: scores of pages.
 //
-// M[g][j] = sum_c max(q_c low_jc, q_c high_jc) for the query heads of a group and every page.  With q split into its positive and its
+// M[g][j] = sum_c max(q_c low_jc, q_c high_jc) for the query heads of a group and every page (the criterion of J. Tang et al., "Quest: query-aware
+// sparsity for efficient long-context LLM inference", 2024).  With q split into its positive and its
 // negative part the maximum is one multiplication and one addition of a product with zero, exact in float32 (products of two 16-bit
 // numbers have at most 22 bits), two channels an instruction; the tree of additions that follows is part of the operator's definition.
 // d/8 lanes take a page (eight channels of minima and maxima each).
 //
-// Bound: memory (4 d bytes a page and KV head), with about as many instructions as the SMs can issue meanwhile: 64 a page for four heads.
+// Bound: memory (4 d bytes a page and KV head); the instructions, 64 a page for four heads, take the SMs some three quarters of that time.
 // All rows -- (request, KV head, four heads) -- lie one behind the other and every warp takes an equal run of pages, copied asynchronously into a
 // ring of its own.  (One cluster of CTAs a row, which kept the sums in shared memory and picked the pages as well: 24 contexts of 300 to 64K
 // tokens in 16-token pages 52 us.)  What picks the pages is decode_pick.cu.
